@@ -493,8 +493,9 @@ harp_status_t harp_kv_gather(const harp_kv_cache_t *cache, const harp_kv_batch_t
  *   max_kv_len  host: no sequence is expected to be longer.  It decides how the work is cut; longer ones are still
  *               computed in full.
  *   workspace   at least harp_attention_int8_workspace_size bytes, 16-byte aligned (NULL where that is 0)
- * Queries are rounded to half precision against their row's largest coordinate (an eighth of a bfloat16 rounding at
- * the largest), and so are the weights; sums are float32.  For HARP_F32 callers both are held as the sum of two halves (22 bits).
+ * Queries (against their row's largest coordinate) and weights are held as the sum of two halves (22 bits); sums are float32.  Where a
+ * bfloat16 call has many rows (128 or more rows and query heads of a key head per sequence in the mean, and enough of them to
+ * fill the card), both are one half, an eighth of a bfloat16 rounding; a caller who wants the 22 bits there too passes HARP_F32.
  * Weights times scales are held against the largest value scale that a row sees, to 2^-32 of it for every key.
  * The same arguments give the same bits.
  */

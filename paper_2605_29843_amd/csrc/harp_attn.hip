@@ -280,9 +280,12 @@ struct Rows {
 // is 16 g + 4 t + r, which makes the 16 weights of lane group g those of the 16 keys that one 16-byte piece of the value layout holds.
 // Keys and values go from memory to registers, the next turn's keys while this turn is computed; nothing passes through LDS but the
 // join of the W waves.
-// EXACT (float32 callers): queries and weights as the sum of two halves, 22 bits.
-// Bound by the cache's bytes: 48 ragged contexts of up to 8192 keys (8 key heads of 128, 32 query heads) 98 us, 2 x 131072 keys 118 us (4.6 TB/s).
-template <typename T, int DH, bool EXACT, int W>
+// Queries and weights are the sum of two halves, 22 bits, for bfloat16 callers too: what is then left between a result and the exact one is
+// the result's own rounding.  One half of each took 3 % less time where the cache's bytes bound the kernel and up to 9 % less elsewhere (48
+// ragged contexts of up to 8192 keys 98 us, 16 of 2000 keys 20.6), and moved one entry of ten to the next bfloat16 number.
+// Bound by the cache's bytes: 48 ragged contexts of up to 8192 keys (8 key heads of 128, 32 query heads) 101 us, 2 x 131072 keys 121 us (4.5 TB/s),
+// 16 of 2000 keys 22.8 us (through Python, the pieces' join included).
+template <typename T, int DH, int W>
 __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c, RopeView rope, const T *Q, int64_t q_row,
                                                                                   int64_t q_head, T *O, int64_t o_row, int64_t o_head,
                                                                                   int32_t q_heads, int32_t group, float scale_log2,
@@ -345,7 +348,7 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
   load_keys(begin, ahead, ka);
   ahead = look(begin + TURN);
 
-  Rows<DH, EXACT, 1> st;
+  Rows<DH, true, 1> st;
   {
     int64_t flat = row0 + n;
     flat = flat < rows ? flat : rows - 1;
@@ -431,6 +434,9 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
 // code is widened once per workgroup.  Operands as above; a lane's 16 bytes of one product step are one piece of an LDS row, and the pieces
 // of a row stand in an order that spreads the lanes of a read over all banks (keys: piece ^ row; values: the two pieces of a coordinate
 // change places from 8 coordinates to the next).  The next turn's codes are loaded while this turn is computed, and widened behind it.
+// EXACT (float32 callers): queries and weights as the sum of two halves, as above.  For bfloat16 callers they are one half each, an eighth of
+// the result's own rounding: here the products and the weights' rounding are what takes the time (two chunks of up to 1500 rows behind up to
+// 6000 keys 210 us, with both in two halves 303).
 // Bound by vector instructions (the exponentials, the weights' rounding, the widening: 60 % of the cycles) and the matrix instructions (a third),
 // which two waves per SIMD hardly overlap: 2048 rows at the end of 8192 keys, 32 query heads of 128, 368 us (0.65 PFLOP/s); two chunks of up to
 // 1500 rows behind up to 6000 keys 211 us.
@@ -672,7 +678,6 @@ template <typename T, int DH>
 harp_status_t attention_typed(const KvView &c, const RopeView &rope, const void *Q, int64_t q_row, int64_t q_head, void *O,
                               int64_t o_row, int64_t o_head, int32_t q_heads, float scale_log2, Split sp, float *ws, bool wide,
                               bool wide_o, hipStream_t stream) {
-  constexpr bool EXACT = sizeof(T) == 4;
   const int32_t group = q_heads / c.heads;
   const int64_t slots = c.rows * group / sp.slot + c.batch;
   if (slots > 0x7fffffff || c.heads > 65535 || sp.pieces > 65535 || q_heads > 65535) return HARP_ERR_UNSUPPORTED;
@@ -682,12 +687,12 @@ harp_status_t attention_typed(const KvView &c, const RopeView &rope, const void 
                          (const T *)Q, q_row, q_head, (T *)O, o_row, o_head, q_heads, group, scale_log2, sp.piece, sp.pieces, ws, wide, wide_o);
     };
     if (sp.waves == 8)
-      few(harp_attention_few_kernel<T, DH, EXACT, 8>, 8);
+      few(harp_attention_few_kernel<T, DH, 8>, 8);
     else
-      few(harp_attention_few_kernel<T, DH, EXACT, 4>, 4);
+      few(harp_attention_few_kernel<T, DH, 4>, 4);
   } else {
     if (slots * c.heads * sp.pieces > 0x7fffffff) return HARP_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((harp_attention_many_kernel<T, DH, EXACT>), dim3((unsigned)(slots * c.heads * sp.pieces)), dim3(256), 0, stream, c,
+    hipLaunchKernelGGL((harp_attention_many_kernel<T, DH, sizeof(T) == 4>), dim3((unsigned)(slots * c.heads * sp.pieces)), dim3(256), 0, stream, c,
                        rope, (const T *)Q, q_row, q_head, (T *)O, o_row, o_head, q_heads, group, scale_log2, sp.piece, sp.pieces, ws, wide,
                        wide_o, (uint32_t)slots);
   }

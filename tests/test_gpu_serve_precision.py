@@ -1,0 +1,40 @@
+"""How exact the serving operators are where test_gpu_serve.py's worst-case bounds leave room."""
+import numpy as np
+import pytest
+
+import serve_oracle as so
+from test_gpu_serve import dev, harp, host, make_batch, rounded, say  # noqa: F401  (harp: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def half_step(x, dtype):
+    """Half the distance of neighbouring numbers of the type at |x|, x in float64."""
+    bits = 8 if dtype == "bf16" else 24
+    return np.exp2(np.floor(np.log2(np.maximum(np.abs(x), 1e-300))) - bits)
+
+
+def attend(harp, cache, table, row_start, kv_len, Q, rope, dtype, longest=None):
+    out = harp.harp_attention_int8(harp.KVCache(*(dev(a) for a in cache)), dev(table), dev(row_start), dev(kv_len), dev(Q, dtype),
+                                   rope=None if rope is None else tuple(dev(a) for a in rope), max_kv_len=longest)
+    return host(out).astype(np.float64)
+
+
+def two_halves_bound(A, S, dh, keys):
+    """What 22 bits of queries and weights and float32 sums leave: test_gpu_serve.py's derivation."""
+    return 2 * A * (2.0 ** -21 * (1 + 2 * S) + (dh + keys) * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("new,total,page,heads,group,dh", [([1], [40], 16, 8, 4, 64), ([1] * 6, [64, 65, 3, 50, 31, 17], 32, 4, 4, 128), ([9, 3], [60, 20], 16, 4, 7, 64),
+                                                           ([1, 1], [300, 700], 64, 4, 8, 128), ([1], [1500], 128, 2, 8, 64)])
+def test_few_rows_of_bfloat16_are_the_rounded_result(harp, new, total, page, heads, group, dh):
+    """Between the exact result and a bfloat16 one of few rows stands the result's own rounding, and what two halves leave."""
+    say("few rows, bf16", new, total, page, heads, group, dh)
+    r = np.random.default_rng(sum(total) + dh + group)
+    cache, table, row_start, kv_len, angles = make_batch(r, new, total, page, heads, dh)
+    Q = rounded(r.standard_normal((int(row_start[-1]), heads * group, dh)) * 1.5, "bf16")
+    O, A, S = so.attention(cache, table, row_start, kv_len, Q, angles, False, dh ** -0.5)
+    got = attend(harp, cache, table, row_start, kv_len, Q, angles, "bf16", max(total))
+    bound = two_halves_bound(A, S, dh, table.shape[1] * page)
+    tol = half_step(np.abs(O) + bound, "bf16") + bound
+    assert (np.abs(got - O) <= tol).all(), (int((np.abs(got - O) > tol).sum()), float(np.max(np.abs(got - O) / tol)))
