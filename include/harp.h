@@ -496,7 +496,8 @@ harp_status_t harp_kv_gather(const harp_kv_cache_t *cache, const harp_kv_batch_t
  * Queries (against their row's largest coordinate) and weights are held as the sum of two halves (22 bits); sums are float32.  Where a
  * bfloat16 call has many rows (128 or more rows and query heads of a key head per sequence in the mean, and enough of them to
  * fill the card), both are one half, an eighth of a bfloat16 rounding; a caller who wants the 22 bits there too passes HARP_F32.
- * Weights times scales are held against the largest value scale that a row sees, to 2^-32 of it for every key.
+ * Weights times value scales are held against the largest value scale that a row sees: two halves to 2^-39 of it for every key (so
+ * with all their bits where the scales of the pages that count are within 2^17 of each other), one half to 2^-32.
  * The same arguments give the same bits.
  */
 harp_status_t harp_attention_int8_workspace_size(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch,

@@ -19,9 +19,6 @@ typedef __attribute__((address_space(1))) const void gptr_t;
 typedef __attribute__((address_space(3))) void lptr_t;
 
 constexpr int kWaves = 4;
-// Weights are exp2(s - m + 7), m being the largest score or one that the largest has passed by less than 8: sums are rescaled only
-// where it has passed by more, and half precision still has 2^-21 of the largest at full precision.
-constexpr float kWeightLog = 7.f, kSlack = 8.f;
 
 __device__ __forceinline__ f4 mfma_h(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
@@ -121,8 +118,13 @@ __device__ __forceinline__ void load_query(const T *q, int d0, bool wide, const 
 }
 
 // The running state of R tiles of 16 rows; a lane has row n of each.
+// Weights are exp2(s - m + kWeightLog), m being the largest score or one that the largest has passed by less than kSlack: sums are rescaled
+// only where it has passed by more.  They end below 2^15, and half precision at 2^-24, so one half has 2^-21 of the largest weight at full
+// precision.  The sum of two halves keeps its 22 bits to 2^-17 of the largest weight times its value scale, which is what it is there for, so it
+// rescales more often (2048 rows behind 6144 keys, float32 438 -> 448 us; few rows the same).
 template <int DH, bool EXACT, int R>
 struct Rows {
+  static constexpr float kSlack = EXACT ? 1.f : 8.f, kWeightLog = 15.f - kSlack;
   h8 qh[R][DH / 32], ql[EXACT ? R : 1][DH / 32];   // queries over a power of two, as one half or the sum of two
   float row_scale[R];                              // not negative: what a product is a score's (base 2) of
   int32_t pos[R];                                  // keys 0 .. pos are visible

@@ -38,3 +38,27 @@ def test_few_rows_of_bfloat16_are_the_rounded_result(harp, new, total, page, hea
     bound = two_halves_bound(A, S, dh, table.shape[1] * page)
     tol = half_step(np.abs(O) + bound, "bf16") + bound
     assert (np.abs(got - O) <= tol).all(), (int((np.abs(got - O) > tol).sum()), float(np.max(np.abs(got - O) / tol)))
+
+
+@pytest.mark.parametrize("new,heads", [(1, 1), (129, 28)])
+@pytest.mark.parametrize("apart", [8, 16, 18, 20])
+def test_float32_pages_of_very_different_magnitudes(harp, apart, new, heads):
+    """The first page's values are 2^apart times as large and its keys weigh 2^-apart as much, so both count alike.  Scores come from one
+    product each, exact but for three roundings of a score of `apart` (base 2); sums of n keys and the 22 bits add."""
+    say("scales apart", apart, new, heads)
+    r = np.random.default_rng(apart)
+    dh, total = 64, max(new + 3, 32)
+    cache, table, row_start, kv_len, _ = make_batch(r, [new], [total], 16, heads, dh)
+    k, v, ks, vs = cache
+    k[:], ks[:], vs[:] = 0, 1, r.uniform(0.5, 1, vs.shape)
+    k[table[0, 0], :, :, 0] = -127
+    ks[table[0, 0]] = apart * np.log(2) / 127
+    vs[table[0, 0]] *= 2.0 ** apart
+    Q = np.zeros((new, 4 * heads, dh), np.float32)
+    Q[:, :, 0] = 1
+    O, A, _ = so.attention(cache, table, row_start, kv_len, Q, None, False, 1.0)
+    out = harp.harp_attention_int8(harp.KVCache(*(dev(a) for a in cache)), dev(table), dev(row_start), dev(kv_len), dev(Q), scale=1.0, max_kv_len=total)
+    keys = (total - new + 1 + np.arange(new))[:, None, None]
+    tol = 2.0 ** -23 * np.abs(O) + 2 * A * 2.0 ** -24 * (8 + 4 * apart + keys)
+    off = np.abs(host(out) - O)
+    assert (off <= tol).all(), float(np.max(off / tol))
