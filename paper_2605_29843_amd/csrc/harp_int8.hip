@@ -444,12 +444,19 @@ __global__ __launch_bounds__(256) void harp_matmul_int8_join_kernel(const int32_
     if (ch + r < d_out) sv_put(Y + tok * ldy + ch + r, scaled(sum[r], st, sw[ch + r]));
 }
 
+// Rows of one launch: a launch has fewer than 2^32 threads in a dimension (rows of 1024 threads: fewer than 2^22 rows).
+constexpr int64_t kMostRows = 1 << 21;
+
 template <typename T>
 harp_status_t quantize_typed(const T *X, int64_t ldx, int64_t n, int64_t d, int8_t *codes, int64_t ldc, float *scales,
                              bool wide_in, bool wide_out, hipStream_t stream) {
   auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(threads), 0, stream, X, ldx, d, codes, ldc, scales, wide_in, wide_out);
-    return hipGetLastError() == hipSuccess ? HARP_OK : HARP_ERR_DEVICE;
+    for (int64_t i = 0; i < n; i += kMostRows) {
+      const unsigned rows = (unsigned)(n - i < kMostRows ? n - i : kMostRows);
+      hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, stream, X + i * ldx, ldx, d, codes + i * ldc, ldc, scales + i, wide_in, wide_out);
+      if (hipGetLastError() != hipSuccess) return HARP_ERR_DEVICE;
+    }
+    return HARP_OK;
   };
   // 1024 threads a row, up to one row per compute unit (48 rows of 14336: 5.5 us, with 256 threads 10.7) and for rows that 256 threads
   // would hold in too many registers.
