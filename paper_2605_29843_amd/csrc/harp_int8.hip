@@ -522,13 +522,13 @@ MatmulPlan choose_matmul(int64_t n, int64_t d_out, int64_t d_in) {
 }
 int64_t part_pitch(int64_t d_out) { return (d_out + 15) / 16 * 16; }
 
+// One launch's part of a product (and the join of its slices)
 template <typename T>
-harp_status_t matmul_typed(MatmulPlan plan, const int8_t *A, int64_t lda, const float *sa, const int8_t *W, int64_t ldw, const float *sw,
+harp_status_t matmul_part(MatmulPlan plan, const int8_t *A, int64_t lda, const float *sa, const int8_t *W, int64_t ldw, const float *sw,
                            int64_t n, int64_t d_out, int64_t d_in, T *Y, int64_t ldy, int32_t *parts, hipStream_t stream) {
   auto status = [] { return hipGetLastError() == hipSuccess ? HARP_OK : HARP_ERR_DEVICE; };
   auto tiles = [&](auto kernel, int bm, int bn, int threads) {
     const int64_t tm = (n + bm - 1) / bm, tn = (d_out + bn - 1) / bn;
-    if (tm * tn > 0x7fffffff) return HARP_ERR_UNSUPPORTED;
     const bool wide_y = (uintptr_t)Y % 16 == 0 && ldy * sizeof(T) % 16 == 0;
     const int32_t steps = (int32_t)((d_in + 127) / 128), slice = (steps + plan.slices - 1) / plan.slices;
     const int64_t ldp = part_pitch(d_out);
@@ -543,9 +543,7 @@ harp_status_t matmul_typed(MatmulPlan plan, const int8_t *A, int64_t lda, const 
     return st;
   };
   auto few = [&](auto kernel) {
-    const int64_t groups = (d_out + 15) / 16;
-    if (groups > 0x7fffffff) return HARP_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(512), 0, stream, A, lda, sa, W, ldw, sw, n, d_out, d_in, Y, ldy);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((d_out + 15) / 16)), dim3(512), 0, stream, A, lda, sa, W, ldw, sw, n, d_out, d_in, Y, ldy);
     return status();
   };
   switch (plan.kernel) {
@@ -557,11 +555,26 @@ harp_status_t matmul_typed(MatmulPlan plan, const int8_t *A, int64_t lda, const 
     case k256x256: return tiles(harp_matmul_int8_tile_kernel<T, 256, 256, 2, 4>, 256, 256, 512);
     case kAny: break;
   }
-  const int64_t gx = (d_out + 63) / 64, gy = (n + 63) / 64;
-  if (gx > 0x7fffffff || gy > 65535) return HARP_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(harp_matmul_int8_any_kernel<T>, dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, A, lda, sa, W, ldw,
-                     sw, n, d_out, d_in, Y, ldy);
+  hipLaunchKernelGGL(harp_matmul_int8_any_kernel<T>, dim3((unsigned)((d_out + 63) / 64), (unsigned)((n + 63) / 64)), dim3(256), 0, stream,
+                     A, lda, sa, W, ldw, sw, n, d_out, d_in, Y, ldy);
   return status();
+}
+
+// A launch has fewer than 2^32 threads in x and fewer than 2^16 workgroups in y, so results are computed in parts of up to 2^24 channels and
+// as many rows as make 2^34 results (every tile has 16 results a thread or more), 2^21 at most; rows are whole tiles of every size but in the
+// last part.  Slices (n <= 65535) are joined before the next part's take their places.
+template <typename T>
+harp_status_t matmul_typed(MatmulPlan plan, const int8_t *A, int64_t lda, const float *sa, const int8_t *W, int64_t ldw, const float *sw,
+                           int64_t n, int64_t d_out, int64_t d_in, T *Y, int64_t ldy, int32_t *parts, hipStream_t stream) {
+  const int64_t most_ch = (int64_t)1 << 24, ch = d_out < most_ch ? d_out : most_ch, wide = ch < 256 ? 256 : ch;
+  const int64_t fit = ((int64_t)1 << 34) / wide / 768 * 768, most_rows = fit < kMostRows / 768 * 768 ? fit : kMostRows / 768 * 768;
+  for (int64_t j = 0; j < d_out; j += ch)
+    for (int64_t i = 0; i < n; i += most_rows) {
+      const harp_status_t st = matmul_part(plan, A + i * lda, lda, sa + i, W + j * ldw, ldw, sw + j, n - i < most_rows ? n - i : most_rows,
+                                           d_out - j < ch ? d_out - j : ch, d_in, Y + i * ldy + j, ldy, parts, stream);
+      if (st != HARP_OK) return st;
+    }
+  return HARP_OK;
 }
 
 // Tiles are addressed from their first row with 32 bits.

@@ -27,3 +27,21 @@ def test_quantize_more_rows_than_a_launch_has(harp, n, d, dtype):
     codes, scales = dev(codes), dev(scales)
     assert bool((out[:whole].view(-1, period, d) == codes).all()) and torch.equal(out[whole:], codes[:n - whole])
     assert bool((s[:whole].view(-1, period) == scales).all()) and torch.equal(s[whole:], scales[:n - whole])
+
+
+@pytest.mark.parametrize("n,d_out,d_in,pitch", [(65535 * 64 + 70, 3, 5, 5), ((1 << 21) + 5, 20, 32, 32), (2, (1 << 24) + 40, 16, 16),
+                                                (40, (1 << 24) + 40, 16, 16), (40, (1 << 24) + 40, 5, 7)])
+def test_products_in_more_than_one_part(harp, n, d_out, d_in, pitch):
+    """More than 2^16 tiles of 64 unaligned rows, more rows and more channels than one launch takes.  Sums are below 2^24: exact in float32."""
+    import torch
+    say("matmul", n, d_out, d_in, pitch)
+    g = torch.Generator(device="cuda").manual_seed(n % 1000 + d_in)
+    codes = lambda rows: torch.randint(-128, 128, (rows, pitch), device="cuda", generator=g, dtype=torch.int8)[:, :d_in]   # noqa: E731
+    scale = lambda rows: torch.rand(rows, device="cuda", generator=g) + 0.5   # noqa: E731
+    a, sa, w, sw = codes(n), scale(n), codes(d_out), scale(d_out)
+    y = torch.full((n, d_out), 3.0, dtype=torch.bfloat16, device="cuda")
+    harp.harp_matmul_int8(a, sa, w, sw, y)
+    for j in range(0, d_out, 1 << 20):      # (the library's product of 2^24 columns at once has wrong sums)
+        part = slice(j, j + (1 << 20))
+        sums = a.float().contiguous() @ w[part].float().t().contiguous()
+        assert torch.equal(y[:, part], ((sums * sa[:, None]) * sw[part]).bfloat16())
