@@ -408,10 +408,11 @@ harp_status_t harp_quantize_rows(const void *X, int64_t ldx, int64_t n, int64_t 
  * Y[i, j] = (sum_k A[i, k] * W[j, k]) * a_scales[i] * w_scales[j],   i < n, j < d_out, k < d_in.
  * The sum is exact (int32); it is rounded to float32, multiplied by the scales in this order and rounded once
  * to dt.  A: codes [n, d_in], pitch lda; W: codes [d_out, d_in], pitch ldw; Y: [n, d_out] of type dt, pitch
- * ldy.  Any alignment and any sizes up to d_in <= HARP_INT8_MAX_DEPTH (HARP_ERR_UNSUPPORTED beyond); operands whose
- * addresses and pitches are multiples of 16 are read 16 codes at a time, others code by code.
+ * ldy.  Any alignment and any sizes up to d_in <= HARP_INT8_MAX_DEPTH (HARP_ERR_UNSUPPORTED beyond).  Operands whose
+ * addresses and pitches are multiples of 16 (and pitches below 2^23) are copied in whole pieces by the fast kernels; others have a slower one.
  *   workspace   at least harp_matmul_int8_workspace_size bytes, 16-byte aligned (NULL where that is 0): int32 sums of
- *               slices of k, where n and d_out alone make too few tiles.  Nothing in it has to be initialised.
+ *               slices of k, where n and d_out alone make too few tiles.  Nothing in it has to be initialised.  Other than such
+ *               operands need none.
  */
 harp_status_t harp_matmul_int8_workspace_size(int64_t n, int64_t d_out, int64_t d_in, size_t *bytes);
 harp_status_t harp_matmul_int8(const int8_t *A, int64_t lda, const float *a_scales, const int8_t *W, int64_t ldw,

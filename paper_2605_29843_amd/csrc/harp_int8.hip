@@ -521,6 +521,9 @@ MatmulPlan choose_matmul(int64_t n, int64_t d_out, int64_t d_in) {
   return best;
 }
 int64_t part_pitch(int64_t d_out) { return (d_out + 15) / 16 * 16; }
+size_t parts_bytes(MatmulPlan plan, int64_t n, int64_t d_out) {
+  return plan.slices > 1 ? (size_t)plan.slices * n * part_pitch(d_out) * sizeof(int32_t) : 0;
+}
 
 // One launch's part of a product (and the join of its slices)
 template <typename T>
@@ -604,8 +607,7 @@ harp_status_t harp_quantize_rows(const void *X, int64_t ldx, int64_t n, int64_t 
 harp_status_t harp_matmul_int8_workspace_size(int64_t n, int64_t d_out, int64_t d_in, size_t *bytes) {
   if (n < 0 || d_out < 0 || d_in < 1 || !bytes) return HARP_ERR_INVALID_ARG;
   if (d_in > HARP_INT8_MAX_DEPTH) return HARP_ERR_UNSUPPORTED;
-  const harp::MatmulPlan plan = harp::choose_matmul(n, d_out, d_in);
-  *bytes = plan.slices > 1 ? (size_t)plan.slices * n * harp::part_pitch(d_out) * sizeof(int32_t) : 0;
+  *bytes = harp::parts_bytes(harp::choose_matmul(n, d_out, d_in), n, d_out);
   return HARP_OK;
 }
 
@@ -616,12 +618,11 @@ harp_status_t harp_matmul_int8(const int8_t *A, int64_t lda, const float *a_scal
     return HARP_ERR_INVALID_ARG;
   if (n == 0 || d_out == 0) return HARP_OK;
   if (!A || !a_scales || !W || !w_scales || !Y) return HARP_ERR_INVALID_ARG;
-  size_t need = 0;
-  const harp_status_t st = harp_matmul_int8_workspace_size(n, d_out, d_in, &need);
-  if (st != HARP_OK) return st;
-  if (need && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16)) return HARP_ERR_INVALID_ARG;
+  if (d_in > HARP_INT8_MAX_DEPTH) return HARP_ERR_UNSUPPORTED;
   const harp::MatmulPlan plan = harp::matmul_aligned(A, lda, W, ldw) ? harp::choose_matmul(n, d_out, d_in)
                                                                      : harp::MatmulPlan{n <= 32 ? harp::kFew : harp::kAny, 1};
+  const size_t need = harp::parts_bytes(plan, n, d_out);
+  if (need && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16)) return HARP_ERR_INVALID_ARG;
   if (dt == HARP_F32)
     return harp::matmul_typed(plan, A, lda, a_scales, W, ldw, w_scales, n, d_out, d_in, (float *)Y, ldy, (int32_t *)workspace,
                               (hipStream_t)stream);

@@ -45,3 +45,17 @@ def test_products_in_more_than_one_part(harp, n, d_out, d_in, pitch):
         part = slice(j, j + (1 << 20))
         sums = a.float().contiguous() @ w[part].float().t().contiguous()
         assert torch.equal(y[:, part], ((sums * sa[:, None]) * sw[part]).bfloat16())
+
+
+def test_unaligned_products_need_no_workspace(harp):
+    """Sizes that are cut into slices where the operands are aligned; the kernel of unaligned ones has no slices."""
+    import torch
+    n, d_out, d_in = 48, 256, 2048
+    r = np.random.default_rng(3)
+    a, w = (dev(r.integers(-128, 128, (rows, d_in + 1)).astype(np.int8)) for rows in (n, d_out))
+    sa, sw, y = torch.ones(n, device="cuda"), torch.ones(d_out, device="cuda"), torch.zeros(n, d_out, device="cuda")
+    assert harp.harp_matmul_int8_workspace_size(n, d_out, d_in) > 0
+    status = harp.lib.harp_matmul_int8(a.data_ptr(), d_in + 1, sa.data_ptr(), w.data_ptr(), d_in + 1, sw.data_ptr(), n, d_out, d_in, y.data_ptr(),
+                                       d_out, harp.HARP_F32, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert status == harp.HARP_OK
+    assert np.array_equal(host(y), so.matmul(host(a[:, :d_in]), np.ones(n, np.float32), host(w[:, :d_in]), np.ones(d_out, np.float32)))
