@@ -415,6 +415,8 @@ harp_status_t harp_quantize_rows(const void *X, int64_t ldx, int64_t n, int64_t 
  *               operands need none.
  */
 harp_status_t harp_matmul_int8_workspace_size(int64_t n, int64_t d_out, int64_t d_in, size_t *bytes);
+/* Short name of the kernel that aligned operands of these sizes take (static string; "none" for sizes that are refused). */
+const char *harp_matmul_int8_kernel_name(int64_t n, int64_t d_out, int64_t d_in);
 harp_status_t harp_matmul_int8(const int8_t *A, int64_t lda, const float *a_scales, const int8_t *W, int64_t ldw,
                                const float *w_scales, int64_t n, int64_t d_out, int64_t d_in, void *Y, int64_t ldy,
                                harp_dtype_t dt, void *workspace, size_t workspace_bytes, void *stream);
@@ -503,6 +505,8 @@ harp_status_t harp_kv_gather(const harp_kv_cache_t *cache, const harp_kv_batch_t
  */
 harp_status_t harp_attention_int8_workspace_size(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch,
                                                  int32_t q_heads, int64_t max_kv_len, size_t *bytes);
+/* Short name of the kernel that such a call takes, "..._pieces" if contexts are cut (static string; "none" for refused arguments). */
+const char *harp_attention_int8_kernel_name(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch, int32_t q_heads, int64_t max_kv_len);
 harp_status_t harp_attention_int8(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch, const void *Q,
                                   int64_t q_row, int64_t q_head, void *O, int64_t o_row, int64_t o_head,
                                   int32_t q_heads, harp_dtype_t dt, float scale, const harp_rope_t *rope,

@@ -743,6 +743,14 @@ harp_status_t harp_attention_int8_workspace_size(const harp_kv_cache_t *cache, c
   return st;
 }
 
+const char *harp_attention_int8_kernel_name(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch, int32_t q_heads, int64_t max_kv_len) {
+  harp::KvView c;
+  harp::Split sp;
+  size_t need = 0;
+  if (harp::attention_args(cache, batch, q_heads, max_kv_len, &c, &sp, &need) != HARP_OK) return "none";
+  return sp.slot == 16 ? (sp.pieces > 1 ? "few_rows_pieces" : "few_rows") : (sp.pieces > 1 ? "many_rows_pieces" : "many_rows");
+}
+
 harp_status_t harp_attention_int8(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch, const void *Q, int64_t q_row,
                                   int64_t q_head, void *O, int64_t o_row, int64_t o_head, int32_t q_heads, harp_dtype_t dt,
                                   float scale, const harp_rope_t *rope, int64_t max_kv_len, void *workspace,

@@ -470,7 +470,7 @@ harp_status_t quantize_typed(const T *X, int64_t ldx, int64_t n, int64_t d, int8
   return go(harp_quantize_rows_kernel<T, 256, 4>, 256);
 }
 
-enum MatmulKernel { kAny, kFew, k32x128, k64x64, k128x128, k192x256, k256x256 };
+enum MatmulKernel { kAny, kFew, k32x128, k64x64, k128x128, k192x256, k256x256 };   // (harp_matmul_int8_kernel_name names them in this order)
 struct MatmulPlan {
   MatmulKernel kernel;
   int32_t slices;   // of the sums over k, joined by a second launch
@@ -609,6 +609,15 @@ harp_status_t harp_matmul_int8_workspace_size(int64_t n, int64_t d_out, int64_t 
   if (d_in > HARP_INT8_MAX_DEPTH) return HARP_ERR_UNSUPPORTED;
   *bytes = harp::parts_bytes(harp::choose_matmul(n, d_out, d_in), n, d_out);
   return HARP_OK;
+}
+
+const char *harp_matmul_int8_kernel_name(int64_t n, int64_t d_out, int64_t d_in) {
+  if (n < 0 || d_out < 0 || d_in < 1 || d_in > HARP_INT8_MAX_DEPTH) return "none";
+  static const char *const kNames[][2] = {{"any", nullptr}, {"few", nullptr}, {"tile_32x128", "tile_32x128_sliced"}, {"tile_64x64", "tile_64x64_sliced"},
+                                          {"tile_128x128", "tile_128x128_sliced"}, {"tile_192x256", "tile_192x256_sliced"},
+                                          {"tile_256x256", "tile_256x256_sliced"}};
+  const harp::MatmulPlan plan = harp::choose_matmul(n, d_out, d_in);
+  return kNames[plan.kernel][plan.slices > 1];
 }
 
 harp_status_t harp_matmul_int8(const int8_t *A, int64_t lda, const float *a_scales, const int8_t *W, int64_t ldw,

@@ -86,10 +86,12 @@ _SIGS = {
                                 _sz, _vp]),
     "harp_quantize_rows": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _vp]),
     "harp_matmul_int8_workspace_size": (_i32, [_i64, _i64, _i64, C.POINTER(_sz)]),
+    "harp_matmul_int8_kernel_name": (C.c_char_p, [_i64, _i64, _i64]),
     "harp_matmul_int8": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i32, _vp, _sz, _vp]),
     "harp_kv_append": (_i32, [_cache_p, _batch_p, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _rope_p, _vp]),
     "harp_kv_gather": (_i32, [_cache_p, _batch_p, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _vp]),
     "harp_attention_int8_workspace_size": (_i32, [_cache_p, _batch_p, _i32, _i64, C.POINTER(_sz)]),
+    "harp_attention_int8_kernel_name": (C.c_char_p, [_cache_p, _batch_p, _i32, _i64]),
     "harp_attention_int8": (_i32, [_cache_p, _batch_p, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _i32, C.c_float,
                                    _rope_p, _i64, _vp, _sz, _vp]),
     "harp_greedy_schedule": (_i32, [_i64, _i32, _i32, C.POINTER(_i32), C.POINTER(_i32)]),
@@ -597,6 +599,10 @@ def harp_matmul_int8_workspace_size(n: int, d_out: int, d_in: int) -> int:
     return int(need.value)
 
 
+def harp_matmul_int8_kernel_name(n: int, d_out: int, d_in: int) -> str:
+    return lib.harp_matmul_int8_kernel_name(int(n), int(d_out), int(d_in)).decode()
+
+
 def _workspace(workspace, need: int, like, stream):
     """(tensor, address, bytes); the caller's, or a new one on the device of `like` where some is needed"""
     if workspace is None:
@@ -744,6 +750,13 @@ def harp_attention_int8_workspace_size(cache, page_table, row_start, kv_len, row
     _check(lib.harp_attention_int8_workspace_size(args, batch, int(q_heads), longest, need),
            "harp_attention_int8_workspace_size")
     return int(need.value)
+
+
+def harp_attention_int8_kernel_name(cache, page_table, row_start, kv_len, rows: int, q_heads: int,
+                                    max_kv_len: int | None = None) -> str:
+    args, batch = _cache_args(cache), _batch_args(page_table, row_start, kv_len, int(rows))
+    longest = batch.max_pages * args.page_size if max_kv_len is None else int(max_kv_len)
+    return lib.harp_attention_int8_kernel_name(args, batch, int(q_heads), longest).decode()
 
 
 def harp_attention_int8(cache, page_table, row_start, kv_len, Q, out=None, scale: float | None = None, rope=None,

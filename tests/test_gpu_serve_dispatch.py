@@ -1,0 +1,37 @@
+"""The serving operators where the choice of a kernel decides what is computed how: test_serve_dispatch.py says which kernels these sizes reach."""
+import numpy as np
+import pytest
+
+import serve_oracle as so
+from test_gpu_serve import check_attention, dev, harp, host, make_batch, rounded, say  # noqa: F401  (harp: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n,d_out,d_in", [(700, 4100, 16400)])
+def test_matmul_largest_tiles_in_slices(harp, n, d_out, d_in):
+    import torch
+    say("matmul", n, d_out, d_in)
+    r = np.random.default_rng(n + d_out)
+    a, w = r.integers(-128, 128, (n, d_in)).astype(np.int8), r.integers(-128, 128, (d_out, d_in)).astype(np.int8)
+    sa, sw = r.uniform(0.01, 2, n).astype(np.float32), r.uniform(0.01, 2, d_out).astype(np.float32)
+    want = so.matmul(a, sa, w, sw)
+    for dtype, td in (("f32", torch.float32), ("bf16", torch.bfloat16)):
+        assert np.array_equal(host(harp.harp_matmul_int8(dev(a), dev(sa), dev(w), dev(sw), dtype=td)), rounded(want, dtype)), dtype
+
+
+# Rows at negative positions, whole tiles of them, and a sequence whose only page is not there, in every attention kernel
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,total,page,heads,group,dh", [([200, 300, 130], [100, 330, 16], 16, 28, 2, 64), ([300, 130], [200, 16], 32, 28, 2, 128),
+                                                           ([200, 130, 129], [100, 1300, 16], 64, 8, 4, 128), ([260, 150], [100, 1400], 16, 16, 2, 64),
+                                                           ([130, 9, 2], [2, 40, 16], 16, 2, 1, 64), ([140, 3], [12, 90], 32, 1, 1, 128),
+                                                           ([150, 2], [6, 1500], 64, 1, 1, 64), ([1, 135], [2000, 5], 128, 2, 1, 128)])
+def test_attention_rows_without_keys(harp, new, total, page, heads, group, dh, dtype):
+    say("rows without keys", new, total, page, heads, group, dh, dtype)
+    r = np.random.default_rng(sum(total) + page + dh)
+    cache, table, row_start, kv_len, angles = make_batch(r, new, total, page, heads, dh, missing=((len(new) - 1, 0, -1),) if total[-1] == 16 else ())
+    Q = rounded(r.standard_normal((int(row_start[-1]), heads * group, dh)) * 1.5, dtype)
+    out = host(check_attention(harp, cache, table, row_start, kv_len, Q, angles, dh == 64, dtype, longest=max(total)))
+    for b, (n, t) in enumerate(zip(new, total)):
+        none = n if total[-1] == 16 and b == len(new) - 1 else max(n - t, 0)
+        assert not out[row_start[b]:row_start[b] + none].any()
