@@ -62,3 +62,43 @@ def test_float32_pages_of_very_different_magnitudes(harp, apart, new, heads):
     tol = 2.0 ** -23 * np.abs(O) + 2 * A * 2.0 ** -24 * (8 + 4 * apart + keys)
     off = np.abs(host(out) - O)
     assert (off <= tol).all(), float(np.max(off / tol))
+
+
+def spread(cache, table, row_start, kv_len, Q, scale):
+    """(O, E) in float64: the result, and the r.m.s. that independent roundings of queries and weights to one half (each within 2^-11 of itself,
+    r.m.s. 2^-11 / sqrt(3) at most) leave in it.  A score's is s_j^2 = sum_i (q_i k_ij scale)^2 2^-22 / 3; it moves the weight in both sums, so o by
+    w_j (V_j - o) times it.  The sum of weights is taken before they are rounded, so a weight's own rounding moves o by w_j V_j times it."""
+    _, heads, size, dh = cache[0].shape
+    group = Q.shape[1] // heads
+    O, E = np.zeros(Q.shape), np.zeros(Q.shape)
+    for b in range(len(kv_len)):
+        total, n = int(kv_len[b]), int(row_start[b + 1] - row_start[b])
+        K, V, there = so.tokens(cache, table, b, total)
+        assert there.all()
+        for j in range(n):
+            see, t = total - n + j + 1, int(row_start[b]) + j
+            for h in range(Q.shape[1]):
+                k, v, x = K[:see, h // group], V[:see, h // group], Q[t, h].astype(np.float64) * scale
+                w = np.exp(k @ x - (k @ x).max())
+                w /= w.sum()
+                o = w @ v
+                c = w * w * ((k * k) @ (x * x))
+                moved = np.maximum(c @ (v * v) - 2 * o * (c @ v) + o * o * c.sum(), 0) + (w * w) @ (v * v)
+                O[t, h], E[t, h] = o, np.sqrt(moved * 2.0 ** -22 / 3)
+    return O, E
+
+
+@pytest.mark.parametrize("new,total,page,heads,group,dh", [([600], [600], 128, 8, 3, 64), ([130], [2600], 64, 7, 4, 128), ([300, 200], [300, 450], 32, 8, 4, 128),
+                                                           ([128], [4000], 32, 1, 16, 64), ([1], [9000], 32, 1, 4, 64), ([2, 1, 1], [1500, 900, 64], 16, 4, 4, 128)])
+def test_bfloat16_errors_are_those_of_independent_roundings(harp, new, total, page, heads, group, dh):
+    """No entry is further off than half a step of bfloat16 and six times the r.m.s. of what the roundings leave (of 10^6 normal numbers one
+    in a thousand runs has one beyond), and all together not further than their r.m.s.  The roundings to one half bound what two halves leave, too."""
+    say("errors", new, total, page, heads, group, dh)
+    r, dtype = np.random.default_rng(sum(total) + dh), "bf16"
+    cache, table, row_start, kv_len, _ = make_batch(r, new, total, page, heads, dh)
+    Q = rounded(r.standard_normal((int(row_start[-1]), heads * group, dh)) * 0.7, dtype)
+    O, E = spread(cache, table, row_start, kv_len, Q, dh ** -0.5)
+    off = np.abs(attend(harp, cache, table, row_start, kv_len, Q, None, dtype, max(total)) - O)
+    h = half_step(np.abs(O) + 6 * E, dtype)
+    assert (off <= h + 6 * E).all(), float(np.max(off / (h + 6 * E)))
+    assert np.mean(off ** 2) <= 1.1 * np.mean(h ** 2 / 3 + E ** 2), float(np.mean(off ** 2) / np.mean(h ** 2 / 3 + E ** 2))
