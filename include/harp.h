@@ -460,7 +460,7 @@ typedef struct {
 /*
  * Position rotation: at position p the pair (a, b) of coordinates becomes (a cos - b sin, b cos + a sin) with
  * cos[p * head_dim / 2 + i], sin[...] for pair i: coordinates (i, i + head_dim / 2), or (2 i, 2 i + 1) if interleaved
- * is 1.  The float32 tables (device) hold at least max_pages * page_size positions.  Host structure; a NULL pointer in its
+ * is 1.  The float32 tables (device) hold at least max_pages * page_size positions (NULL where that is 0).  Host structure; a NULL pointer in its
  * place means no rotation.
  */
 typedef struct {

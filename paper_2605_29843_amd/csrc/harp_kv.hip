@@ -412,7 +412,9 @@ harp_status_t kv_view(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch
 harp_status_t rope_view(const harp_rope_t *rope, const KvView &kv, RopeView *v) {
   *v = {nullptr, nullptr, 0};
   if (!rope) return HARP_OK;
-  if (!rope->cos || !rope->sin || rope->positions < kv.cap || (rope->interleaved != 0 && rope->interleaved != 1)) return HARP_ERR_INVALID_ARG;
+  if (rope->positions < kv.cap || (rope->interleaved != 0 && rope->interleaved != 1)) return HARP_ERR_INVALID_ARG;
+  if (kv.cap == 0) return HARP_OK;   // no position: the tables may be empty, and nothing is read from them
+  if (!rope->cos || !rope->sin) return HARP_ERR_INVALID_ARG;
   *v = {rope->cos, rope->sin, rope->interleaved};
   return HARP_OK;
 }

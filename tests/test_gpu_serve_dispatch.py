@@ -35,3 +35,21 @@ def test_attention_rows_without_keys(harp, new, total, page, heads, group, dh, d
     for b, (n, t) in enumerate(zip(new, total)):
         none = n if total[-1] == 16 and b == len(new) - 1 else max(n - t, 0)
         assert not out[row_start[b]:row_start[b] + none].any()
+
+
+@pytest.mark.parametrize("new,heads", [([3, 2], 1), ([200, 90], 28)])
+def test_no_pages_at_all(harp, new, heads):
+    """A table of no columns and a rotation of no positions: no row has a place, results are zeros and nothing is read or stored."""
+    import torch
+    rows = sum(new)
+    row_start, kv_len = dev(np.cumsum([0] + new).astype(np.int32)), dev(np.zeros(2, np.int32))
+    table = torch.zeros(2, 0, dtype=torch.int32, device="cuda")
+    rope = torch.zeros(0, 32, device="cuda"), torch.zeros(0, 32, device="cuda")
+    c = harp.kv_cache(2, heads, 64, 16)
+    c.k_scale.fill_(3)
+    x = torch.ones(rows, 2 * heads, 64, device="cuda")
+    out = torch.full_like(x, 7.0)
+    harp.harp_kv_append(c, table, row_start, kv_len, x[:, :heads], x[:, heads:], rope=rope)
+    harp.harp_attention_int8(c, table, row_start, kv_len, x, out, rope=rope)
+    assert not bool(out.any()) and bool((c.k_scale == 3).all())
+    assert not any(bool(t.any()) for t in harp.harp_kv_gather(c, table, row_start, kv_len, rows))

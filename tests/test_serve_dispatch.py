@@ -54,3 +54,11 @@ def test_names_of_refused_arguments():
 @pytest.mark.parametrize("n,name", [(1, "few"), (2048, "tile_192x256")])
 def test_product_names(n, name):
     assert harp.harp_matmul_int8_kernel_name(n, 11008, 4096) == name
+
+
+def test_a_table_without_pages_takes_a_rotation_without_positions():
+    cache, batch = harp._CacheArgs(P, P, P, P, 3, 2, 64, 16), harp._BatchArgs(None, 0, P, P, 0, 2, 0)
+    for rope, status in ((harp._RopeArgs(None, None, 0, 0), harp.HARP_OK), (harp._RopeArgs(None, None, 0, 2), harp.HARP_ERR_INVALID_ARG),
+                         (harp._RopeArgs(None, None, -1, 0), harp.HARP_ERR_INVALID_ARG)):
+        assert harp.lib.harp_attention_int8(cache, batch, None, 256, 64, None, 256, 64, 4, 1, 0.1, rope, 0, None, 0, None) == status
+        assert harp.lib.harp_kv_append(cache, batch, None, 128, 64, None, 128, 64, 1, rope, None) == status
