@@ -491,7 +491,7 @@ harp_status_t harp_kv_gather(const harp_kv_cache_t *cache, const harp_kv_batch_t
  * Attention of the batch's rows over the cache (which holds them already, see harp_kv_append):
  *     O[t, h] = sum_p w_p V_p,   w = softmax over p <= position of t of   scale * <rope(Q[t, h]), K_p>,
  * K_p, V_p of key head h / (q_heads / kv_heads).  Q, O [rows, q_heads, head_dim] of type dt, inner stride 1.  A row
- * that sees no key is all zeros.  Hidden keys do not count, whatever their codes and scales hold.
+ * that sees no key is all zeros; one with an infinity or a NaN in its query that sees a key is NaN.  Hidden keys do not count, whatever their codes and scales hold.
  *   rope        rotation of Q (NULL: Q is rotated already, or not at all)
  *   max_kv_len  host: no sequence is expected to be longer.  It decides how the work is cut; longer ones are still
  *               computed in full.

@@ -149,7 +149,8 @@ struct Rows {
     int e = top > 0.f && sv_finite(top) ? 13 - exponent(top) : 0;
     e = e > 126 ? 126 : e;
     const float up = scale_log2 < 0.f ? -pow2i(e) : pow2i(e);
-    row_scale[r] = fabsf(scale_log2) * pow2i(-e);
+    // (an infinite query: every score is infinite or NaN, and scores of one sign only would leave weights of 0 and a sum of 0, as without a key)
+    row_scale[r] = top == __builtin_inff() ? __uint_as_float(0x7fc00000u) : fabsf(scale_log2) * pow2i(-e);
 #pragma unroll
     for (int s = 0; s < DH / 32; ++s)
 #pragma unroll

@@ -53,3 +53,19 @@ def test_no_pages_at_all(harp, new, heads):
     harp.harp_attention_int8(c, table, row_start, kv_len, x, out, rope=rope)
     assert not bool(out.any()) and bool((c.k_scale == 3).all())
     assert not any(bool(t.any()) for t in harp.harp_kv_gather(c, table, row_start, kv_len, rows))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,total,heads", [([3], [40], 2), ([140, 150], [130, 170], 28)])
+def test_an_infinite_query_is_nan(harp, new, total, heads, dtype):
+    """Softmax of scores that are all -inf has no value; results are NaN as for a NaN query, not the zeros of a row without keys."""
+    r = np.random.default_rng(15)
+    cache, table, row_start, kv_len, _ = make_batch(r, new, total, 16, heads, 64)
+    np.clip(np.abs(cache[0]), 1, 127, out=cache[0])                 # no key has a coordinate of 0
+    Q = rounded(r.standard_normal((sum(new), 4 * heads, 64)), dtype)
+    Q[1, 0, 5], Q[-1, 1, 7], Q[-1, 2, 9] = -np.inf, np.inf, -np.inf
+    with np.errstate(invalid="ignore"):
+        O, _, _ = so.attention(cache, table, row_start, kv_len, Q, None, False, 0.125)
+    out = host(harp.harp_attention_int8(harp.KVCache(*(dev(a) for a in cache)), dev(table), dev(row_start), dev(kv_len), dev(Q, dtype)))
+    assert np.array_equal(np.isnan(out), np.isnan(O)) and np.isnan(out).any()
+    assert np.isnan(out[-1, 1]).all() and np.isnan(out[-1, 2]).all() and not np.isnan(out[-1, 0]).any()
