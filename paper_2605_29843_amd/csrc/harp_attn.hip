@@ -125,6 +125,7 @@ __device__ __forceinline__ void load_query(const T *q, int d0, bool wide, const 
 template <int DH, bool EXACT, int R>
 struct Rows {
   static constexpr float kSlack = EXACT ? 1.f : 8.f, kWeightLog = 15.f - kSlack;
+  static constexpr float kOut = 0x1p-15f;   // parts are joined as sums of weights up to 1: at 2^15 the sums of large values would pass the range
   h8 qh[R][DH / 32], ql[EXACT ? R : 1][DH / 32];   // queries over a power of two, as one half or the sum of two
   float row_scale[R];                              // not negative: what a product is a score's (base 2) of
   int32_t pos[R];                                  // keys 0 .. pos are visible
@@ -399,7 +400,7 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
   float top = lds_m[0][n];
 #pragma unroll
   for (int w = 1; w < W; ++w) top = fmaxf(top, lds_m[w][n]);
-  const float fac = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
+  const float fac = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top)) * st.kOut;
   if (g == 0) lds_l[wave][n] = l * fac;
 #pragma unroll
   for (int v = 0; v < VB; ++v) *(f4 *)&lds[(wave * 16 + n) * PITCH + 16 * v + 4 * g] = st.acc[0][v] * (fac * st.unit[0]);
@@ -589,8 +590,8 @@ __global__ __launch_bounds__(256, 2) void harp_attention_many_kernel(KvView c, R
     } else {
       float *part = ws + ((row * q_heads + h) * pieces + z) * (DH + 4);
 #pragma unroll
-      for (int v = 0; v < VB; ++v) *(f4 *)(part + 16 * v + 4 * g) = st.acc[r][v] * st.unit[r];
-      if (g == 0) part[DH] = st.m[r], part[DH + 1] = den, part[DH + 2] = __int_as_float(used_pieces(slot_most, piece, pieces));
+      for (int v = 0; v < VB; ++v) *(f4 *)(part + 16 * v + 4 * g) = st.acc[r][v] * (st.kOut * st.unit[r]);
+      if (g == 0) part[DH] = st.m[r], part[DH + 1] = st.kOut * den, part[DH + 2] = __int_as_float(used_pieces(slot_most, piece, pieces));
     }
   }
 }

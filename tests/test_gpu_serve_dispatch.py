@@ -69,3 +69,15 @@ def test_an_infinite_query_is_nan(harp, new, total, heads, dtype):
     out = host(harp.harp_attention_int8(harp.KVCache(*(dev(a) for a in cache)), dev(table), dev(row_start), dev(kv_len), dev(Q, dtype)))
     assert np.array_equal(np.isnan(out), np.isnan(O)) and np.isnan(out).any()
     assert np.isnan(out[-1, 1]).all() and np.isnan(out[-1, 2]).all() and not np.isnan(out[-1, 0]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [2.0 ** 115, 1e-29])
+@pytest.mark.parametrize("new,total,heads,group", [([1], [400], 1, 4), ([1], [700], 1, 4), ([1], [6000], 1, 2), ([130], [1300], 28, 2), ([260], [300], 28, 2)])
+def test_attention_of_very_large_and_small_values(harp, new, total, heads, group, size, dtype):
+    """Values near 2^117, whose sums over the keys stay within float32, and ones of 10^-29: few rows by four waves and eight, many rows, pieces of both."""
+    r = np.random.default_rng(16)
+    cache, table, row_start, kv_len, angles = make_batch(r, new, total, 64, heads, 64)
+    cache[3][...] *= np.float32(size)
+    Q = rounded(r.standard_normal((sum(new), heads * group, 64)), dtype)
+    check_attention(harp, cache, table, row_start, kv_len, Q, angles, False, dtype, longest=max(total))
