@@ -426,7 +426,7 @@ harp_status_t harp_matmul_int8(const int8_t *A, int64_t lda, const float *a_scal
  *   k        [pages, kv_heads, page_size, head_dim]
  *   v        [pages, kv_heads, page_size / 16, head_dim, 16]: the codes that one coordinate has for 16
  *            consecutive tokens lie beside each other, as the product with attention weights takes them
- *   k_scale, v_scale   [pages, kv_heads], none of them negative
+ *   k_scale, v_scale   [pages, kv_heads], none of them negative; value scales below 2^126 (an append makes none above 2^122)
  * Dense arrays, k and v aligned to 16 bytes; nothing in them has to be initialised.  page_size is 16, 32, 64 or
  * 128 and head_dim 64 or 128 (HARP_ERR_UNSUPPORTED otherwise).  The structure itself is host memory.
  */

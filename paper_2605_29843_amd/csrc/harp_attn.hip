@@ -121,7 +121,7 @@ __device__ __forceinline__ void load_query(const T *q, int d0, bool wide, const 
 // Weights are exp2(s - m + kWeightLog), m being the largest score or one that the largest has passed by less than kSlack: sums are rescaled
 // only where it has passed by more.  They end below 2^15, and half precision at 2^-24, so one half has 2^-21 of the largest weight at full
 // precision.  The sum of two halves keeps its 22 bits to 2^-17 of the largest weight times its value scale, which is what it is there for, so it
-// rescales more often (2048 rows behind 6144 keys, float32 438 -> 448 us; few rows the same).
+// rescales more often (2048 rows at the end of 8192 keys, float32: 448 us, with a slack of 8 438; few rows the same).
 template <int DH, bool EXACT, int R>
 struct Rows {
   static constexpr float kSlack = EXACT ? 1.f : 8.f, kWeightLog = 15.f - kSlack;
@@ -288,7 +288,7 @@ struct Rows {
 // the result's own rounding.  One half of each took 3 % less time where the cache's bytes bound the kernel and up to 9 % less elsewhere (48
 // ragged contexts of up to 8192 keys 98 us, 16 of 2000 keys 20.6), and moved one entry of ten to the next bfloat16 number.
 // Bound by the cache's bytes: 48 ragged contexts of up to 8192 keys (8 key heads of 128, 32 query heads) 101 us, 2 x 131072 keys 121 us (4.5 TB/s),
-// 16 of 2000 keys 22.8 us (through Python, the pieces' join included).
+// 16 of 2000 keys 23 us, one of 700 keys 11.5 us.
 template <typename T, int DH, int W>
 __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c, RopeView rope, const T *Q, int64_t q_row,
                                                                                   int64_t q_head, T *O, int64_t o_row, int64_t o_head,
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
   }
 
   const bool whole = pieces == 1 || (piece >= most && z == 0);
-  // join of the four waves
+  // join of the waves
   __shared__ __align__(16) float lds[W * 16 * PITCH];
   __shared__ float lds_m[W][16], lds_l[W][16];
   const float m = st.m[0], l = over_groups_sum(st.l[0]);
@@ -442,8 +442,8 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
 // the result's own rounding: here the products and the weights' rounding are what takes the time (two chunks of up to 1500 rows behind up to
 // 6000 keys 210 us, with both in two halves 303).
 // Bound by vector instructions (the exponentials, the weights' rounding, the widening: 60 % of the cycles) and the matrix instructions (a third),
-// which two waves per SIMD hardly overlap: 2048 rows at the end of 8192 keys, 32 query heads of 128, 368 us (0.65 PFLOP/s); two chunks of up to
-// 1500 rows behind up to 6000 keys 211 us.
+// which two waves per SIMD hardly overlap: 2048 rows at the end of 8192 keys, 32 query heads of 128, 289 us (0.83 PFLOP/s; float32 452), heads of
+// 64 201 us; two chunks of up to 1500 rows behind up to 6000 keys 210 us (float32 323).
 template <typename T, int DH, bool EXACT>
 __global__ __launch_bounds__(256, 2) void harp_attention_many_kernel(KvView c, RopeView rope, const T *Q, int64_t q_row, int64_t q_head,
                                                                      T *O, int64_t o_row, int64_t o_head, int32_t q_heads, int32_t group,
@@ -647,21 +647,25 @@ __global__ __launch_bounds__(256) void harp_attention_join_kernel(KvView c, T *O
 struct Split {
   int32_t slot, piece, pieces, waves;
 };
-// Many rows: from 128 rows a sequence in the mean on (contexts of 8192 keys, 8 key heads of 128, 4 sequences, with 64, 128 and 256 rows each:
-// few 58, 90, 146 us, many 58, 70, 86; float32 60, 94, 155 and 70, 88, 114), if that makes 112 workgroups or more: fewer leave more of the
-// card idle than they save (128 rows behind 1000 keys, 8 workgroups: few 13 us, many 34; 1024 rows, 64: 20 and 34; 4 x 512 rows, 128: 38 and 34; 256 rows
-// behind 4000 keys, 112 in pieces: 33 and 29).
-// Keys are cut into pieces of 512 or more until there are so many workgroups: 512 of the large ones (4 x 8192 keys, 2048 rows each: 334 us, with
-// 1024 workgroups 353, and 512 rows each 109 and 122), 1536 of the small ones where a sequence has one tile of rows (48 ragged contexts of
-// up to 8192 keys: 98 us, with 768 workgroups 105), 768 where it has more tiles and every piece costs their joining (16 x 2048
-// keys, 64 rows each: 32 us, with 1536 workgroups 39).  Few keys are one piece, since a second launch costs the host 5 us:
-// up to 1024 (one sequence, kernels alone: 1024 keys 11.5 us; 1100 keys 11.8 in three pieces, 12.5 in one), up to 2048 with one tile
-// of rows for each of 16 sequences and 8 heads or more (16 x 2000 keys 19 us, in four pieces 24; 64 ragged contexts of up to 2000 keys 34, in
-// three 44; 64 x 2000 keys 57 and 53).  Where so short pieces still leave compute units idle, they have 256 keys, one turn of the four waves
-// (one sequence of 2000 keys: 10.1 us, in pieces of 512 12.3).
+// Many rows: from 128 rows of a key head and sequence in the mean on (contexts of 8192 keys, 8 key heads of 128, 4 sequences, with 64, 128 and
+// 256 such rows each: few 64, 99, 158 us, many 63, 79, 95; float32 65, 99, 156 and 77, 103, 129), if that makes 112 workgroups or more: fewer
+// leave more of the card idle than they save (128 rows behind 1000 keys, 8 workgroups: few 16 us, many 37; 1024 rows, 64: 24 and 37; 4 x 512
+// rows, 128: 44 and 40; 256 rows behind 4000 keys, 112 in pieces: 38 and 33).  The mean is what the host knows: where few sequences have nearly
+// all of the rows, the others' workgroups are the wrong ones (2048 rows at 4000 keys beside 31 sequences of one row, in many-row workgroups: 256 us,
+// the two parts alone 138 and 68; beside 80, in few-row ones: 455, alone 138 and 147).
+// Keys are cut into pieces of 512 or more until there are so many workgroups: 512 of the large ones (4 x 8192 keys, 2048 rows each: 316 us, with
+// 1024 workgroups 341, and 512 rows each 100 and 121), 1536 of the small ones where a sequence has one tile of rows (48 ragged contexts of
+// up to 8192 keys: 101 us, with 768 workgroups 106), 768 where it has more tiles and every piece costs their joining (16 x 2048
+// keys, 32 rows each: 41 us, with 1536 workgroups 44).  All sequences have pieces of one length, from the longest that is announced: one of 131072 keys
+// among 63 of 1000 takes 618 us, alone 72.  Few keys are one piece, since a second launch costs the host 5 us:
+// up to 1024 (one sequence, kernels alone: 1024 keys 14.0 us; 1100 keys 11.2 in five pieces, 15.4 in one), up to 2048 with one tile
+// of rows for each of 16 sequences and 8 heads or more (16 x 2000 keys 23 us, in four pieces 28; 64 ragged contexts of up to 2000 keys 48, in
+// three 56; 64 x 2000 keys 72 and 70).  Where so short pieces still leave compute units idle, they have 256 keys, one turn of the four waves
+// (one sequence of 2000 keys: 11.1 us, in pieces of 512 13.7).
 // One piece of more than 512 keys and a compute unit for every workgroup: eight waves take it, since a turn of 64 keys per wave is 2.2 us of
-// waiting for memory (kernel alone: one sequence of 700 keys 9.4 us, with four waves 10.7; 16 of 2000 keys 19 and 27; up to 512 keys
-// four waves are 1 us faster).
+// waiting for memory (kernel alone: one sequence of 700 keys 11.5 us, with four waves 12.9; 16 of 2000 keys 23 and 29; of 512 keys 10.2 both,
+// 300 keys 10.4 and 9.8; 288 workgroups of up to 1900 keys, float32: 20.7 and 19.5).
+// (Launches back to back in a graph, inputs of three calls in turn, the join of pieces included.)
 Split choose_split(int64_t rows, int32_t batch, int32_t group, int32_t heads, int64_t max_kv) {
   const int64_t per = batch > 0 ? rows * group / batch : 0;
   for (bool many = per >= 128;; many = false) {

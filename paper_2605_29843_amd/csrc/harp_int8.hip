@@ -12,8 +12,9 @@ typedef int32_t i4v __attribute__((ext_vector_type(4)));
 
 // ---- one row per workgroup: s = max |x| / 127, q = rint(x / s)
 // The row stays in registers between the two passes (NV pieces of 8 values per thread), so it is read once.  Bound by those bytes where there
-// are many rows (16384 x 8192 bf16 75 us, 4096 x 28672 67 us: 5.3 TB/s; 2048 x 4096 5.5 us), by the way through one row where there are
-// few (1 x 4096 2.5 us, 48 x 14336 3.5 us).
+// are many rows (16384 x 8192 bf16 74 us, 4096 x 28672 65 us: 5.4 TB/s; 2048 x 4096 6.8 us), by the way through one row where there are
+// few (1 x 4096 2.3 us, 48 x 14336 3.3 us).  (Here and below: launches back to back in a graph, operands of three calls in turn, so that small
+// ones stand in the last-level cache; traced launch by launch the shortest kernels take up to half as long again.)
 template <typename T, int TH, int NV>
 __global__ __launch_bounds__(TH) void harp_quantize_rows_kernel(const T *X, int64_t ldx, int64_t d, int8_t *codes, int64_t ldc,
                                                                  float *scales, bool wide_in, bool wide_out) {
@@ -116,7 +117,7 @@ __device__ __forceinline__ sv_u4 load_cut(const int8_t *p, int64_t count) {
 
 // Any alignment and pitch: tiles of 64 channels x 64 tokens, steps of 128 codes through registers into LDS, the next step's loads in flight
 // while this step is multiplied.  Copies straight into LDS, which the tiles below are made of, need aligned pieces.  Bound by the loads, which
-// cross lines: 2048 x 4096 x 4096 at an odd address 135 us, aligned (in tiles) 45.
+// cross lines: 2048 x 4096 x 4096 at an odd address 135 us, aligned (in tiles) 37.
 template <typename T>
 __global__ __launch_bounds__(256) void harp_matmul_int8_any_kernel(const int8_t *A, int64_t lda, const float *sa, const int8_t *W,
                                                                    int64_t ldw, const float *sw, int64_t n, int64_t d_out,
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(256) void harp_matmul_int8_any_kernel(const int8_t 
 // copy puts lane i at place i, so it is the address that is exchanged.  A step is 128 codes because eight lanes then ask for one
 // whole line of 128 bytes: with steps of 64 codes the same tiles took 10 to 25 % longer.  The rows of a tile of the weight are taken in the
 // order that leaves 4 TN neighbouring channels of one token in a lane.
-// Bound by power: 4096 x 8192 x 28672 takes 771 us (2500 TOP/s) on random codes and a quarter less on zeros.
+// Bound by power: 4096 x 8192 x 28672 takes 770 us (2500 TOP/s) on random codes and 684 on zeros.
 typedef __attribute__((address_space(1))) const void gptr_t;
 typedef __attribute__((address_space(3))) void lptr_t;
 
@@ -368,8 +369,8 @@ __global__ __launch_bounds__(64 * WT * WC) void harp_matmul_int8_tile_kernel(con
 }
 
 // Few tokens: the weight is read once, straight into registers, by waves that share a tile of 16 channels x 16 RT tokens and divide its
-// sums among them; their parts meet in LDS.  Any alignment.  Bound by the weight's bytes: 4096 x 14336, one row, 12.6 us (4.7 TB/s).  Up to 32 tokens; with
-// more, every workgroup's own reading of all of them from L2 takes longer than the weight (48 rows: 31 us, tiles in slices 19 us).
+// sums among them; their parts meet in LDS.  Any alignment.  Bound by the weight's bytes: 4096 x 14336, one row, 12.3 us (4.8 TB/s).  Up to 32 tokens; with
+// more, every workgroup's own reading of all of them from L2 takes longer than the weight (32 rows: 22 us, tiles in slices 18 us).
 template <typename T, int RT>
 __global__ __launch_bounds__(512) void harp_matmul_int8_few_kernel(const int8_t *A, int64_t lda, const float *sa, const int8_t *W,
                                                                    int64_t ldw, const float *sw, int64_t n, int64_t d_out,
@@ -458,7 +459,7 @@ harp_status_t quantize_typed(const T *X, int64_t ldx, int64_t n, int64_t d, int8
     }
     return HARP_OK;
   };
-  // 1024 threads a row, up to one row per compute unit (48 rows of 14336: 5.5 us, with 256 threads 10.7) and for rows that 256 threads
+  // 1024 threads a row, up to one row per compute unit (48 rows of 14336: 3.3 us, with 256 threads 5.2) and for rows that 256 threads
   // would hold in too many registers.
   if ((n <= 256 && d > 8 * 256) || d > 8 * 1024) {
     const int64_t pieces = (d + 8 * 1024 - 1) / (8 * 1024);
@@ -478,10 +479,11 @@ struct MatmulPlan {
 
 // The kernel is the one whose estimated time is the least.  A tile kernel's time is its steps times what a step takes with p
 // workgroups per compute unit, but no less than its bytes take: measured for n = 1 .. 2048 with weights of 2048 x 8192, 4096 x 4096,
-// 4096 x 14336, 11008 x 4096 and 28672 x 8192; the choice is 3 % slower in the mean than the best of every kernel and number of
-// slices, 22 % at most.  What it chooses between: 4096 x 14336, 48 rows: 64 x 64 tiles 68 us, eight slices of them 19 us (few: 31 us); 2048
-// rows of 11008 x 4096: 192 x 256 tiles 92 us (two rounds of workgroups, nearly full), 256 x 256 102 us (two, one of them a third
-// full), 128 x 128 101 us; 777 rows of 28672 x 8192: 256 x 256 206 us, 128 x 128 248 us; one row of 4096 x 14336: few 12.6 us, tiles 16.7 us.
+// 4096 x 14336, 11008 x 4096 and 28672 x 8192; the choice is 7 % slower in the mean than the best of every kernel and number of
+// slices, 61 % at most (400 rows of 11008 x 4096: 32 x 128 tiles 51 us, 128 x 128 31: five workgroups of the former do not fit a compute
+// unit's LDS).  What it chooses between: 4096 x 14336, 48 rows: 64 x 64 tiles 68 us, 32 x 128 in twelve slices 19 us; 2048
+// rows of 11008 x 4096: 192 x 256 tiles 95 us (two rounds of workgroups, nearly full), 256 x 256 108 us (two, one of them a third
+// full), 128 x 128 108 us; 777 rows of 28672 x 8192: 256 x 256 211 us, 128 x 128 253 us; one row of 4096 x 14336: few 12.3 us, tiles 16.1 us.
 struct TileCost {
   MatmulKernel kernel;
   int bm, bn;

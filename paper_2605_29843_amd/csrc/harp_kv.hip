@@ -84,8 +84,10 @@ __device__ __forceinline__ PageWork page_work(const KvView &c, int64_t &nth) {
 // the pass that finds the largest and the one that rounds them, so inputs are read once, and it alone writes this page's codes of
 // this head.  A thread's piece is 8 values of one token for keys (4 pairs of the rotation), and 16 tokens of VP coordinates for values:
 // those are the 16-byte groups that the value layout keeps together.  What a few tokens cost is the chain of loads that finds the page
-// (rows, table, old scale), so the new values are asked for before the page is known: 64 tokens of 8 heads of 128, 6.4 us.  Many tokens are bound
-// by their bytes in float32 (8 x 2048 tokens 29 us, 5.8 TB/s) and by instructions in bf16 (28 us, 3.6 TB/s).
+// (rows, table, old scale), so the new values are asked for before the page is known: 64 tokens of 8 heads of 128, 6.3 us.  Many tokens: 8 x
+// 2048 tokens 28 us in float32 with inputs and cache in the last-level cache (5.9 TB/s), 39 us with three of them in turn (4.3); bf16 takes
+// as long (27 and 39 us) with 100 MB in place of 168, so not its bytes bound it but the steps from a value to its stored code, 16 loads of two
+// coordinates for each piece of values among them.  (Launches back to back in a graph.)
 template <typename T, int DH, int PAGE>
 __global__ __launch_bounds__(256) void harp_kv_append_kernel(KvView c, RopeView rope, const T *K, int64_t k_row, int64_t k_head,
                                                              const T *V, int64_t v_row, int64_t v_head, bool k_wide, bool v_wide,
@@ -256,7 +258,8 @@ __global__ __launch_bounds__(256) void harp_kv_append_kernel(KvView c, RopeView 
 }
 
 // The last rows of every sequence, code * scale; same workgroups and pieces as the append.  Bound by the bytes (8 x 2048 tokens of 8 heads of
-// 128 18 us, 5.5 TB/s), few tokens by the same chain of loads (64 tokens 4.1 us).  Rows without a place, or on a page that the
+// 128, bf16, 18 us behind the append that wrote them, 24 us with three caches in turn: 4.3 TB/s), few tokens by the same chain of loads (64
+// tokens 4.0 us, 1848 tokens of 64 sequences 6.8).  Rows without a place, or on a page that the
 // table does not name, are zeros.
 template <typename T, int DH, int PAGE>
 __global__ __launch_bounds__(256) void harp_kv_gather_kernel(KvView c, T *K, int64_t k_row, int64_t k_head, T *V, int64_t v_row,
