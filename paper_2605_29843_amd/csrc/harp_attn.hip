@@ -286,7 +286,7 @@ struct Rows {
 // join of the W waves.
 // Queries and weights are the sum of two halves, 22 bits, for bfloat16 callers too: what is then left between a result and the exact one is
 // the result's own rounding.  One half of each took 3 % less time where the cache's bytes bound the kernel and up to 9 % less elsewhere (48
-// ragged contexts of up to 8192 keys 98 us, 16 of 2000 keys 20.6), and moved one entry of ten to the next bfloat16 number.
+// ragged contexts of up to 8192 keys 98 us, 16 of 2000 keys 20.6), and moved one entry of six to the next bfloat16 number.
 // Bound by the cache's bytes: 48 ragged contexts of up to 8192 keys (8 key heads of 128, 32 query heads) 101 us, 2 x 131072 keys 121 us (4.5 TB/s),
 // 16 of 2000 keys 23 us, one of 700 keys 11.5 us.
 template <typename T, int DH, int W>
