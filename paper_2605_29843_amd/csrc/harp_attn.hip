@@ -297,7 +297,7 @@ __global__ __launch_bounds__(64 * W, 2) void harp_attention_few_kernel(KvView c,
   constexpr int KS = DH / 32, VB = DH / 16, PITCH = DH + 4, TURN = 64 * W;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   int64_t nth;
-  const Sequence q = find_sequence(c, blockIdx.x, group, 4, 1, nth);
+  const Sequence q = find_sequence(c, c.slot0 + blockIdx.x, group, 4, 1, nth);
   const int64_t rows = (int64_t)q.count * group;
   const int64_t row0 = nth << 4;   // of token row0 / group
   if (nth < 0 || row0 >= rows) return;
@@ -688,23 +688,24 @@ harp_status_t attention_typed(const KvView &c, const RopeView &rope, const void 
                               bool wide_o, hipStream_t stream) {
   const int32_t group = q_heads / c.heads;
   const int64_t slots = c.rows * group / sp.slot + c.batch;
-  if (slots > 0x7fffffff || c.heads > 65535 || sp.pieces > 65535 || q_heads > 65535) return HARP_ERR_UNSUPPORTED;
+  if (c.heads > 65535 || sp.pieces > 65535 || q_heads > 65535) return HARP_ERR_UNSUPPORTED;
   if (sp.slot == 16) {
     auto few = [&](auto kernel, int waves) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)slots, (unsigned)c.heads, (unsigned)sp.pieces), dim3(64 * waves), 0, stream, c, rope,
-                         (const T *)Q, q_row, q_head, (T *)O, o_row, o_head, q_heads, group, scale_log2, sp.piece, sp.pieces, ws, wide, wide_o);
+      return for_slots(c, slots, [&](const KvView &part, unsigned count) {
+        hipLaunchKernelGGL(kernel, dim3(count, (unsigned)c.heads, (unsigned)sp.pieces), dim3(64 * waves), 0, stream, part, rope, (const T *)Q, q_row,
+                           q_head, (T *)O, o_row, o_head, q_heads, group, scale_log2, sp.piece, sp.pieces, ws, wide, wide_o);
+      });
     };
-    if (sp.waves == 8)
-      few(harp_attention_few_kernel<T, DH, 8>, 8);
-    else
-      few(harp_attention_few_kernel<T, DH, 4>, 4);
+    const harp_status_t st = sp.waves == 8 ? few(harp_attention_few_kernel<T, DH, 8>, 8) : few(harp_attention_few_kernel<T, DH, 4>, 4);
+    if (st != HARP_OK) return st;
   } else {
-    if (slots * c.heads * sp.pieces > 0x7fffffff) return HARP_ERR_UNSUPPORTED;
+    // (256 threads each; so many would have 2^31 results of 64 coordinates and more)
+    if (slots * c.heads * sp.pieces >= 1 << 24) return HARP_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((harp_attention_many_kernel<T, DH, sizeof(T) == 4>), dim3((unsigned)(slots * c.heads * sp.pieces)), dim3(256), 0, stream, c,
                        rope, (const T *)Q, q_row, q_head, (T *)O, o_row, o_head, q_heads, group, scale_log2, sp.piece, sp.pieces, ws, wide,
                        wide_o, (uint32_t)slots);
+    if (hipGetLastError() != hipSuccess) return HARP_ERR_DEVICE;
   }
-  if (hipGetLastError() != hipSuccess) return HARP_ERR_DEVICE;
   if (sp.pieces > 1) {
     const int64_t results = c.rows * q_heads;
     const bool spread = sp.pieces > 16 || (sp.pieces > 2 && results <= 2048);   // (few results: more threads for each)

@@ -70,7 +70,7 @@ struct PageWork {
 template <int PAGE>
 __device__ __forceinline__ PageWork page_work(const KvView &c, int64_t &nth) {
   PageWork w;
-  w.q = find_sequence(c, blockIdx.x, 1, c.page_log, 2, nth);
+  w.q = find_sequence(c, c.slot0 + blockIdx.x, 1, c.page_log, 2, nth);
   w.first = w.q.total - w.q.count;
   const int32_t begin = w.first < 0 ? 0 : w.first;
   w.page0 = ((int64_t)begin / PAGE + nth) * PAGE;
@@ -350,17 +350,19 @@ template <typename T, int DH, int PAGE>
 harp_status_t append_inst(const KvView &c, const RopeView &rope, const void *K, int64_t k_row, int64_t k_head, const void *V,
                           int64_t v_row, int64_t v_head, Wide wide, int64_t slots, hipStream_t stream) {
   constexpr int UNITS = 256 / unit_threads(PAGE, DH);
-  hipLaunchKernelGGL((harp_kv_append_kernel<T, DH, PAGE>), dim3((unsigned)slots, (unsigned)((c.heads + UNITS - 1) / UNITS), 2), dim3(256), 0,
-                     stream, c, rope, (const T *)K, k_row, k_head, (const T *)V, v_row, v_head, wide.k, wide.v, wide.rope);
-  return hipGetLastError() == hipSuccess ? HARP_OK : HARP_ERR_DEVICE;
+  return for_slots(c, slots, [&](const KvView &part, unsigned count) {
+    hipLaunchKernelGGL((harp_kv_append_kernel<T, DH, PAGE>), dim3(count, (unsigned)((c.heads + UNITS - 1) / UNITS), 2), dim3(256), 0, stream,
+                       part, rope, (const T *)K, k_row, k_head, (const T *)V, v_row, v_head, wide.k, wide.v, wide.rope);
+  });
 }
 template <typename T, int DH, int PAGE>
 harp_status_t gather_inst(const KvView &c, const RopeView &, const void *K, int64_t k_row, int64_t k_head, const void *V,
                           int64_t v_row, int64_t v_head, Wide wide, int64_t slots, hipStream_t stream) {
   constexpr int UNITS = 256 / unit_threads(PAGE, DH);
-  hipLaunchKernelGGL((harp_kv_gather_kernel<T, DH, PAGE>), dim3((unsigned)slots, (unsigned)((c.heads + UNITS - 1) / UNITS), 2), dim3(256), 0,
-                     stream, c, (T *)K, k_row, k_head, (T *)V, v_row, v_head, wide.k, wide.v);
-  return hipGetLastError() == hipSuccess ? HARP_OK : HARP_ERR_DEVICE;
+  return for_slots(c, slots, [&](const KvView &part, unsigned count) {
+    hipLaunchKernelGGL((harp_kv_gather_kernel<T, DH, PAGE>), dim3(count, (unsigned)((c.heads + UNITS - 1) / UNITS), 2), dim3(256), 0, stream,
+                       part, (T *)K, k_row, k_head, (T *)V, v_row, v_head, wide.k, wide.v);
+  });
 }
 
 typedef harp_status_t (*KvLaunch)(const KvView &, const RopeView &, const void *, int64_t, int64_t, const void *, int64_t,
@@ -384,7 +386,7 @@ harp_status_t run_kv(int op, const harp_kv_cache_t *cache, const harp_kv_batch_t
   if (st != HARP_OK) return st;
   if (c.rows == 0 || c.batch == 0 || c.heads == 0) return HARP_OK;
   const int64_t slots = (c.rows >> c.page_log) + 2 * (int64_t)c.batch;
-  if (slots > 0x7fffffff || c.heads > 65535) return HARP_ERR_UNSUPPORTED;
+  if (c.heads > 65535) return HARP_ERR_UNSUPPORTED;
   const Wide wide = {heads_aligned(K, k_row, k_head, dt, 16), heads_aligned(V, v_row, v_head, dt, dt == HARP_BF16 ? 4 : 8),
                      ((uintptr_t)r.cos | (uintptr_t)r.sin) % 16 == 0};
   return kLaunch[op][dt == HARP_BF16][cache->head_dim == 128][c.page_log - 4](c, r, K, k_row, k_head, V, v_row, v_head, wide, slots,
@@ -409,6 +411,7 @@ harp_status_t kv_view(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch
   v->pages = cache->pages, v->heads = cache->kv_heads, v->page_log = log;
   v->table = batch->page_table, v->row_start = batch->row_start, v->kv_len = batch->kv_len;
   v->ld_table = batch->ld_table, v->rows = batch->rows, v->batch = batch->batch, v->cap = batch->max_pages * cache->page_size;
+  v->slot0 = 0;
   return HARP_OK;
 }
 

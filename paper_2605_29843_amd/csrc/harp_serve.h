@@ -26,7 +26,11 @@ struct KvView {
   const int32_t *kv_len;      // [batch]
   int64_t ld_table, rows;
   int32_t batch, cap;         // cap = max_pages * page
+  int64_t slot0;              // the slot of a launch's first workgroup
 };
+
+// Slots of one launch: a launch has fewer than 2^32 threads in a dimension, and a slot up to 512.
+constexpr int64_t kMostSlots = 1 << 22;
 
 struct RopeView {
   const float *cos, *sin;   // [positions, dh / 2], or null
@@ -176,6 +180,16 @@ __device__ __forceinline__ Sequence find_sequence(const KvView &c, int64_t slot,
   return q;
 }
 #endif
+
+// Host side: launch(view, slots of it) for all slots, in launches that are not too large.
+template <typename F>
+harp_status_t for_slots(KvView c, int64_t slots, F &&launch) {
+  for (c.slot0 = 0; c.slot0 < slots; c.slot0 += kMostSlots) {
+    launch(c, (unsigned)(slots - c.slot0 < kMostSlots ? slots - c.slot0 : kMostSlots));
+    if (hipGetLastError() != hipSuccess) return HARP_ERR_DEVICE;
+  }
+  return HARP_OK;
+}
 
 // Host side: HARP_OK and the kernels' view, or the error of the arguments.
 harp_status_t kv_view(const harp_kv_cache_t *cache, const harp_kv_batch_t *batch, KvView *view);

@@ -59,3 +59,49 @@ def test_unaligned_products_need_no_workspace(harp):
                                        d_out, harp.HARP_F32, None, 0, torch.cuda.current_stream().cuda_stream)
     assert status == harp.HARP_OK
     assert np.array_equal(host(y), so.matmul(host(a[:, :d_in]), np.ones(n, np.float32), host(w[:, :d_in]), np.ones(d_out, np.float32)))
+
+
+def test_more_sequences_than_a_launch_has_slots(harp):
+    """One new token for each of 2^24 sequences (two slots each in the cache's kernels, one in attention's).  All have one page of 16 tokens, of 251 that they
+    share, for gathers and attention; the appends write a page of their own for each."""
+    import torch
+    batch, shared, dh = (1 << 24) + 5, 251, 64
+    say("sequences", batch)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    starts = torch.arange(batch + 1, dtype=torch.int32, device="cuda")
+    lens = (torch.arange(batch, device="cuda") % shared % 16 + 1).int()
+    table = (torch.arange(batch, device="cuda") % shared).int()[:, None]
+    small = harp.kv_cache(shared, 1, dh, 16)
+    for t in small[:2]:
+        t.copy_(torch.randint(-127, 128, t.shape, device="cuda", generator=g))
+    for t in small[2:]:
+        t.copy_(torch.rand(t.shape, device="cuda", generator=g) * 0.02 + 0.01)
+    first = slice(0, shared)
+
+    def periodic(x, want):
+        whole = batch // shared * shared
+        return torch.equal(x[:whole].view(-1, shared, dh), want.view(1, shared, dh).expand(whole // shared, -1, -1)) and \
+            torch.equal(x[whole:, 0], want[:batch - whole, 0])
+
+    q = torch.randn(shared, 1, dh, device="cuda", generator=g).bfloat16()
+    many = q.repeat(batch // shared + 1, 1, 1)[:batch]
+    out = torch.full_like(many, 7.0)
+    harp.harp_attention_int8(small, table, starts, lens, many, out)
+    want = harp.harp_attention_int8(small, table[first], starts[:shared + 1], lens[first], q)
+    assert periodic(out, want) and bool(torch.isfinite(want).all()) and bool(want.any())
+    k, v = out, torch.full_like(many, 7.0)
+    harp.harp_kv_gather(small, table, starts, lens, batch, k, v)
+    want = harp.harp_kv_gather(small, table[first], starts[:shared + 1], lens[first], shared)
+    assert periodic(k, want[0]) and periodic(v, want[1])
+    del k, v, out
+    own = harp.kv_cache(batch, 1, dh, 16)
+    each = torch.arange(batch, dtype=torch.int32, device="cuda")[:, None]
+    ones = torch.ones(batch, dtype=torch.int32, device="cuda")
+    for t in own:
+        t.zero_()
+    harp.harp_kv_append(own, each, starts, ones, many, many)
+    top = q.float().abs().amax(2) / torch.full((), 127.0, device="cuda")
+    codes = torch.round(q.float()[:, 0] / top).to(torch.int8)
+    whole = batch // shared * shared
+    assert torch.equal(own.k_scale[:whole].view(-1, shared), top.view(1, -1).expand(whole // shared, -1)) and torch.equal(own.k_scale, own.v_scale)
+    assert periodic(own.k[:, :, 0], codes[:, None]) and periodic(own.v[:, :, 0, :, 0], codes[:, None])
